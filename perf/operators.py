@@ -114,8 +114,6 @@ def _draw_route(rng, c, most):
     c["masked"] = rng.choice([0.0, 0.0, 0.1])
     if c["experts"] >= 40 and rng.random() < 0.5:
         c["groups"] = rng.choice([4, 8])
-        if c["experts"] % c["groups"]:  # groups are equal: 60 experts have no 8
-            c["groups"] = 4
         c["top_groups"] = rng.randint(1, c["groups"])
         c["group_top"] = rng.choice([1, 2])
         c["k"] = min(c["k"], c["top_groups"] * (c["experts"] // c["groups"]))
