@@ -77,6 +77,11 @@ struct Best {
   __device__ __forceinline__ V worth(int top) const {
     return top == 2 && second > (V)-INFINITY ? first + second : first;
   }
+  // and of their sizes, which its rounding error goes by; -1 without any
+  __device__ __forceinline__ V size(int top) const {
+    if (!(first > (V)-INFINITY)) return -1;
+    return fabs(first) + (top == 2 && second > (V)-INFINITY ? fabs(second) : (V)0);
+  }
 };
 
 // How the groups' values are found: kNone (no groups), kLanes (a group is a power of two
@@ -94,13 +99,20 @@ struct Shared {
 
 // Float32 values whose order float64 might not share.  A softmax score is at most 1 and off
 // by at most 30 roundings of 2^-24 (the sum of its exponentials has 22 of them), a sigmoid
-// by 4; the value with the bias by one more of its own, and a key leaves out 2^-20 of it:
-// less than 2^-18 max(1, |v|) in all, 2^-19 for sigmoids, and two of them are compared;
-// sums of two scores (not cut) by twice that, or 2^-20.
+// by 4; the value v with the bias by one more of its own: 2 (30 or 4) + 2 |v| roundings for
+// two values, less than 2^-18 max(1, |v|), 2^-20 for sigmoids.  A key leaves out up to
+// 15 * 2^-23 < 2^-19 of a value, downwards from both, so that the difference of two cut
+// values is too large by less than one cut.
 __device__ __forceinline__ float value_margin(bool softmax) { return softmax ? 0x1p-17f : 0x1p-18f; }
-__device__ __forceinline__ float group_margin(bool softmax) { return softmax ? 0x1p-16f : 0x1p-18f; }
 __device__ __forceinline__ bool too_close(float high, float low, float within) {
   return !(high - low > within * fmaxf(1.f, fmaxf(fabsf(high), fabsf(low))));
+}
+// How far a group's float32 value may be off: by those of its two summands and one
+// rounding more, 2 (30 or 4) + 2 size roundings of 2^-24 (2^-18.1 or 2^-20.7 for sizes up to
+// 1, 2^-23 of larger ones), where size is the sum of the summands' own sizes: large biases of
+// opposite signs leave a small sum.
+__device__ __forceinline__ float group_error(bool softmax, float size) {
+  return (softmax ? 0x1p-17f : 0x1p-19f) * fmaxf(1.f, size);
 }
 
 // EPL values of `from` for the experts i EPL .., 0 past the last.
@@ -169,7 +181,15 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
   if constexpr (GROUPS != kNone) {
     const int G = a.opt.n_groups, per = E / G, top_groups = a.opt.top_groups;
     const bool fuzzy = sizeof(V) == 4 && (by_value || a.opt.group_top == 2);
-    uint32_t in = 0, out = 0;  // keys: of the worst group that stays (inverted), of the best that goes
+    // Keys of the least that a group that stays may be worth (inverted), and of the most that
+    // one that goes may be.
+    uint32_t in = 0, out = 0;
+    auto ranked = [&](float own, float size, bool keep) {
+      const float at = size < 0.f ? -INFINITY : fminf(fmaxf(own, -FLT_MAX), FLT_MAX);
+      const float off = size < 0.f ? 0.f : fminf(group_error(softmax, size), FLT_MAX);
+      if (keep) in = max(in, ~key_of(at - off));
+      else out = max(out, key_of(at + off));
+    };
     if constexpr (GROUPS == kLanes) {
       const int wide = per / EPL;  // lanes of a group
       Best<V> best;
@@ -191,10 +211,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
         better += other > own || (other == own && h < g);
       }
       const bool keep = better < top_groups;
-      if (g < G) {
-        if (keep) in = ~key_of((float)own);
-        else out = key_of((float)own);
-      }
+      if (fuzzy && g < G) ranked((float)own, (float)best.size(a.opt.group_top), keep);
       if (!keep) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j) value[j] = -INFINITY;
@@ -207,6 +224,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
         Best<V> best;
         for (int e = g * per; e < (g + 1) * per; ++e) best.join((V)mine.value[e], -INFINITY);
         mine.group[g] = key_of((double)best.worth(a.opt.group_top));
+        if (fuzzy) mine.value[g * per] = (double)best.size(a.opt.group_top);  // read by this lane only
       }
       wave_shares();
       for (int g = i; g < G; g += LANES) {
@@ -218,9 +236,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
         }
         const bool keep = better < top_groups;
         mine.keep[g] = keep;
-        const uint32_t k = key_of((float)value_of(own));
-        if (keep) in = max(in, ~k);
-        else out = max(out, k);
+        if (fuzzy) ranked((float)value_of(own), (float)mine.value[g * per], keep);
       }
       wave_shares();
 #pragma unroll
@@ -233,7 +249,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
       in = max_u32<LANES>(in);
       out = max_u32<LANES>(out);
       if (in != 0 && out != 0 && value_of(out) > -INFINITY)
-        sure = !too_close(value_of(~in), value_of(out), group_margin(softmax));
+        sure = value_of(~in) > value_of(out);
     }
   }
 }

@@ -775,3 +775,47 @@ def test_last_round_of_tiles(dev, counts, o, i):
         want = (rows.double() @ m).repeat_interleave(2, 0)
         size = (rows.double().abs() @ m.abs()).repeat_interleave(2, 0)
         assert bool(((got.double() - want).abs() <= (i + 4) * U * size).all())
+
+
+# -------------------------------------------------- values of mixed size
+
+
+@pytest.mark.parametrize("B", [64.0, 128.0, 1000.0, 1e30])
+@pytest.mark.parametrize("E,per", [(64, 2), (64, 4), (96, 3), (256, 16), (1024, 32)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_route_groups_of_cancelling_biases(dev, E, per, B, score):
+    """Groups whose two best values have biases of opposite sign: their sum is near 1, its
+    float32 error that of the biases' size.  Which groups stay goes by float64."""
+    g = gen(int(B) % 1000 + E)
+    G, n = E // per, 200
+    bias = torch.full((G, per), -4 * B)
+    bias[:, 0], bias[:, 1] = B, -B
+    bias[1::2, :2] = 0.0  # and groups of plain scores between them
+    l = torch.randn(n, G, per, generator=g)
+    if score == "sigmoid":  # sums of scores a few 1e-6 apart
+        first = 0.2 + 0.6 * torch.rand(n, G, generator=g).double()
+        target = 0.9 + (torch.rand(n, 1, generator=g).double() - 0.5) * 0.2
+        apart = torch.argsort(torch.rand(n, G, generator=g), dim=1).double() * 3e-6
+        l[:, :, 0] = torch.logit(first).float()
+        l[:, :, 1] = torch.logit(target + apart - torch.sigmoid(l[:, :, 0].double())).float()
+    l = l.view(n, E)
+    opt = dict(score=score, n_groups=G, top_groups=max(1, G // 4), group_top=2, bias=bias.view(-1))
+    k = min(8, opt["top_groups"] * 2)
+    ids, w = R.choose(l.double(), k, **opt)
+    opt["bias"] = opt["bias"].to(dev)
+    got = ntc.route(l.to(dev), k, **opt)
+    assert torch.equal(got.ids.cpu(), ids)
+    close(got.weights, w, (70 + E + 16) * U * w + 1e-37)
+
+
+def test_route_groups_of_infinite_biases(dev):
+    """+inf is a value like others: above all finite ones, equal to itself."""
+    l = torch.randn(50, 64, generator=gen(3))
+    for per in (2, 4, 8):
+        bias = 0.1 * torch.randn(64, generator=gen(4))
+        bias[[5, 40, 41]] = math.inf
+        bias[[8, 9, 17]] = -math.inf
+        l[::3, 40:48] = -math.inf  # a group of none, beside those of +inf
+        opt = dict(score="sigmoid", n_groups=64 // per, top_groups=3, group_top=2)
+        ids, _ = R.choose(l.double(), 5, bias=bias, **opt)
+        assert torch.equal(ntc.route(l.to(dev), 5, bias=bias.to(dev), **opt).ids.cpu(), ids)
