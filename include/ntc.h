@@ -538,10 +538,11 @@ int ntc_linear(const ntc_linear_layer *layer, const ntc_linear_rows *rows,
                size_t workspace_bytes, void *stream);
 
 /*
- * Gradients of ntc_linear: with dz = dy * act'(z), rounded to the layer's type,
+ * Gradients of ntc_linear: with dz = dy * act'(z), which the two products take rounded to
+ * the layer's type,
  *   dx[t]   = sum over the slots s of row t of W_e(s)^T dz[s]   (the layer's type)
  *   dweight = sum over the slots of each expert of dz[s] x[s / slots_per_row]^T
- *   dbias   = sum over the slots of each expert of dz[s]
+ *   dbias   = sum over the slots of each expert of dz[s], float32 before that rounding
  * dy [n][out_dim] of dy_format (the layer's type or NTC_OUT_F32); z is read from
  * epilogue->pre (not needed for NTC_ACT_NONE; act' at 0 is that of the negative
  * side for the two ReLUs); the other epilogue fields are not used: a

@@ -125,8 +125,8 @@ __global__ __launch_bounds__(kBlock) void clear_rows(const uint32_t *written, in
 // columns, a workgroup's four waves every fourth slot, 16 bytes a lane, two rows on
 // their way.  dz = dy * act'(pre) is rounded to T (its one rounding: the products take
 // 16-bit operands) and goes to rows of round8(dim), the pad zero; slots in no bin have
-// none.  parts[tile][c] = sum of the tile's dz[s][c], as rounded; bias_join adds an
-// expert's tiles in order, without atomics.  Bound by the bytes of dy, pre and dz.
+// none.  parts[tile][c] = sum of the tile's dz[s][c] before that rounding; bias_join adds
+// an expert's tiles in order, without atomics.  Bound by the bytes of dy, pre and dz.
 constexpr int kBiasLog = 6, kBiasTile = 1 << kBiasLog, kRowsAhead = 2;
 
 struct GradArgs {
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kBlock) void through_activation(TileArgs a, GradArg
           if (g.activation != NTC_ACT_NONE)
             d[u][j] *= activation_slope(z[u][j], g.activation, g.slope);
           o.v[j] = c + j < a.rows ? (T)d[u][j] : (T)0.f;
-          sum[j] += (float)o.v[j];
+          sum[j] += d[u][j];  // 0 past the last column
         }
         if (g.dz) *(Run<T, 8, true> *)((T *)g.dz + (int64_t)s * pitch + c) = o;
       }

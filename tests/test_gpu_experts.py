@@ -819,3 +819,31 @@ def test_route_groups_of_infinite_biases(dev):
         opt = dict(score="sigmoid", n_groups=64 // per, top_groups=3, group_top=2)
         ids, _ = R.choose(l.double(), 5, bias=bias, **opt)
         assert torch.equal(ntc.route(l.to(dev), 5, bias=bias.to(dev), **opt).ids.cpu(), ids)
+
+
+# --------------------------------------------------------------------- unrounded sums
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n,o", [(1, 24), (300, 520), (4000, 65)])
+def test_bias_gradient_sums_float32(dev, dtype, n, o):
+    """The sum of dy * act'(pre) before that is rounded to the layer's type for the products."""
+    g = gen(n)
+    x, w = torch.zeros(n, 64, dtype=dtype, device=dev), torch.zeros(o, 64, dtype=dtype, device=dev)
+    pre = torch.randn(n, o, generator=g).to(dtype)
+    ids = torch.randint(0, 3, (n,), generator=g).to(torch.int32)  # experts 0 and 1, 2: none
+    ids[ids == 2] = -1
+    bins = ntc.build_bins(ids.to(dev), torch.arange(2, dtype=torch.int32, device=dev), 2)
+    for act, from_t in (("none", F32), ("gelu", dtype), ("silu", F32), ("leaky_relu", dtype)):
+        dy = torch.randn(n, o, generator=g).to(from_t)
+        opt = dict(pre=None if act == "none" else pre.to(dev), activation=act,
+                   leaky_slope=0.3 if act == "leaky_relu" else None, grad_dtype=F32)
+        dz = dy.double() * (1.0 if act == "none" else R.act_slope(pre.double(), act, 0.3))
+        off = (0.0 if act == "none" else 2.0 ** -18) * dy.double().abs() + 2 * U * dz.abs()
+        one = ntc.linear_backward(dy.to(dev), x, w, **opt).bias
+        each = ntc.linear_backward(dy.to(dev), x, w.expand(2, o, 64).contiguous(), bins=bins,
+                                   **opt).bias
+        for got, at in ((one, torch.arange(n)), (each[0], torch.nonzero(ids == 0).view(-1)),
+                        (each[1], torch.nonzero(ids == 1).view(-1))):
+            tol = off[at].sum(0) + (at.numel() + 2) * U * dz[at].abs().sum(0)
+            close(got, dz[at].sum(0), tol)
