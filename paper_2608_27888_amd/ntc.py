@@ -561,11 +561,20 @@ class _Call:
             raise NtcError(fn, status)
 
 
+def _int32(v, what):
+    """v as the library takes it; ctypes would cut off higher bits."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{what} doesn't fit 32 bits")
+    return v
+
+
 def _route_options(score, renormalize, scale, n_groups=1, top_groups=1, group_top=1):
     if score not in SCORES:
         raise ValueError("score must be 'softmax' or 'sigmoid'")
-    return RouteOptions(SCORES[score], int(bool(renormalize)), float(scale), int(n_groups),
-                        int(top_groups), int(group_top))
+    return RouteOptions(SCORES[score], int(bool(renormalize)), float(scale),
+                        _int32(n_groups, "n_groups"), _int32(top_groups, "top_groups"),
+                        _int32(group_top, "group_top"))
 
 
 @dataclass
@@ -591,7 +600,7 @@ def route(logits: torch.Tensor, k: int, score: str = "softmax",
     bp, _ = call.take(bias, "bias", torch.float32, (E,))
     mp, _ = call.take(mask, "mask", (torch.bool, torch.uint8), (n,))
     opt = _route_options(score, renormalize, scale, n_groups, top_groups, group_top)
-    k = int(k)
+    k = _int32(k, "k")
     if k < 1:
         raise ValueError("k must be at least 1")
     ids, weights = call.empty((n, k), torch.int32), call.empty((n, k), torch.float32)
@@ -635,7 +644,7 @@ def _layer(call, x, weight, bias, bins, slots_per_row):
                          "with bins")
     if x.dtype not in (torch.float16, torch.bfloat16):
         raise ValueError("x must be float16 or bfloat16")
-    if int(slots_per_row) < 1:
+    if _int32(slots_per_row, "slots_per_row") < 1:
         raise ValueError("slots_per_row must be at least 1")
     out_dim, in_dim = weight.shape[-2:]
     if x.shape[1] != in_dim:
@@ -757,7 +766,7 @@ def combine(rows: torch.Tensor, weights: Optional[torch.Tensor] = None,
         out = call.empty((n, dim), rows.dtype)
     op, os_ = call.take(out, "out", rows.dtype, (n, dim))
     call.run("ntc_combine", rp, rs, TYPES[rows.dtype], n, k, dim, wp, ip,
-             int(n_experts or 0), sp, ss, op, os_)
+             _int32(n_experts or 0, "n_experts"), sp, ss, op, os_)
     return out
 
 
@@ -781,7 +790,7 @@ def combine_backward(dout: torch.Tensor, rows: torch.Tensor,
     op, os_ = call.take(drows, "drows", rows.dtype)
     gp, _ = call.take(dweights, "dweights", torch.float32)
     call.run("ntc_combine_backward", dp, ds, rp, rs, TYPES[rows.dtype], n, k, dim, wp, ip,
-             int(n_experts or 0), op, os_, gp)
+             _int32(n_experts or 0, "n_experts"), op, os_, gp)
     return drows, dweights
 
 
@@ -800,4 +809,4 @@ def _slots(rows, weights, ids, n_experts, k):
         raise ValueError("rows must hold k slots of every item")
     if ids is not None and n_experts is None:
         raise ValueError("ids need n_experts")
-    return int(n), int(k)
+    return int(n), _int32(k, "k")

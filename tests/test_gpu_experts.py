@@ -847,3 +847,25 @@ def test_bias_gradient_sums_float32(dev, dtype, n, o):
                         (each[1], torch.nonzero(ids == 1).view(-1))):
             tol = off[at].sum(0) + (at.numel() + 2) * U * dz[at].abs().sum(0)
             close(got, dz[at].sum(0), tol)
+
+
+# ----------------------------------------------------------------- arguments of the binding
+
+
+def test_binding_refuses_numbers_past_32_bits(dev):
+    """They would reach the library as others."""
+    l, rows = torch.zeros(4, 64, device=dev), torch.zeros(8, 16, device=dev)
+    x, w = torch.zeros(0, 64, dtype=BF16, device=dev), torch.zeros(8, 64, dtype=BF16, device=dev)
+    ids = torch.zeros(4, 2, dtype=torch.int32, device=dev)
+    wrap = 1 << 32
+    calls = [lambda: ntc.route(l, 2, n_groups=wrap + 4), lambda: ntc.route(l, 2, group_top=wrap + 1),
+             lambda: ntc.route(l, 2, n_groups=4, top_groups=wrap + 1),
+             lambda: ntc.route(l[:0], wrap + 2),
+             lambda: ntc.linear(x, w, slots_per_row=wrap + 1),
+             lambda: ntc.linear_backward(x[:, :8], x, w, slots_per_row=wrap + 1),
+             lambda: ntc.combine(rows[:0], k=wrap + 2),
+             lambda: ntc.combine(rows, ids=ids, n_experts=wrap + 8),
+             lambda: ntc.combine_backward(rows[:4], rows, ids=ids, n_experts=wrap + 8)]
+    for call in calls:
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
