@@ -202,8 +202,10 @@ __global__ __launch_bounds__(kBlock) void through_activation(TileArgs a, GradArg
   }
 }
 
+// there: the tiles that have parts; only bins that overlap would have more.
 template <class T>
-__global__ __launch_bounds__(kBlock) void bias_join(TileArgs a, const float *parts) {
+__global__ __launch_bounds__(kBlock) void bias_join(TileArgs a, const float *parts,
+                                                    uint32_t there) {
   __shared__ uint32_t first;
   const int expert = blockIdx.y;
   uint32_t tiles = (a.n + kBiasTile - 1) / kBiasTile;
@@ -221,6 +223,7 @@ __global__ __launch_bounds__(kBlock) void bias_join(TileArgs a, const float *par
     tiles = tiles_of(expert);
   }
   __syncthreads();
+  tiles = min(tiles, there - min(first, there));
   const int col = blockIdx.x * kBlock + threadIdx.x;
   if (col >= a.rows) return;
   const float *from = parts + (int64_t)first * a.rows + col;
@@ -551,7 +554,7 @@ int backward(const ntc_linear_layer &l, const ntc_linear_rows &r, const ntc_line
   }
   if (g.dbias) {
     bias_join<T><<<dim3((uint32_t)((l.out_dim + kBlock - 1) / kBlock), (uint32_t)l.n_experts),
-                   kBlock, 0, stream>>>(db, (const float *)ws.bias);
+                   kBlock, 0, stream>>>(db, (const float *)ws.bias, parts.x);
   }
   return hip_status(hipGetLastError());
 }

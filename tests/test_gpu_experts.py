@@ -869,3 +869,41 @@ def test_binding_refuses_numbers_past_32_bits(dev):
     for call in calls:
         with pytest.raises(ValueError, match="32 bits"):
             call()
+
+
+def test_bins_that_overlap(dev):
+    """Offsets that are no binning's (each expert's bin the whole of perm) have no right
+    answer; their calls stay within their buffers, and later ones are as before."""
+    g = gen(7)
+    n, E = 300, 24
+    x, dy = torch.randn(n, 64, generator=g).to(BF16).to(dev), torch.randn(n, 96, generator=g).to(BF16).to(dev)
+    w, pre = torch.randn(E, 96, 64, generator=g).to(BF16).to(dev), torch.randn(n, 96, generator=g).to(BF16).to(dev)
+    ids = torch.randint(0, E, (n,), generator=g).to(torch.int32).to(dev)
+    identity = torch.arange(E, dtype=torch.int32, device=dev)
+    good = ntc.build_bins(ids, identity, E)
+    opt = dict(pre=pre, activation="gelu")
+    want = ntc.linear_backward(dy, x, w, bins=good, **opt)
+    bad = ntc.build_bins(ids, identity, E)
+    bad.bin_offset[0::2] = 0
+    bad.bin_offset[1::2] = bad.capacity
+    got = ntc.linear_backward(dy, x, w, bins=bad, **opt)
+    assert got.bias.shape == (E, 96)
+    got = ntc.linear_backward(dy, x, w, bins=good, **opt)
+    for a, b in ((got.x, want.x), (got.weight, want.weight), (got.bias, want.bias)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("align", [1, 64])
+def test_no_rows_with_bins(dev, align):
+    g = gen(1)
+    w = torch.randn(3, 96, 64, generator=g).to(BF16).to(dev)
+    x, dy = torch.zeros(0, 64, dtype=BF16, device=dev), torch.zeros(0, 96, dtype=BF16, device=dev)
+    r = ntc.route(torch.zeros(0, 3, device=dev), 2)
+    assert r.ids.shape == (0, 2)
+    bins = ntc.build_bins(r.ids, torch.arange(3, dtype=torch.int32, device=dev), 3, align=align)
+    assert ntc.linear(x, w, bins=bins, slots_per_row=2).shape == (0, 96)
+    grads = ntc.linear_backward(dy, x, w, bins=bins, slots_per_row=2)
+    assert grads.x.shape == (0, 64) and not bool(grads.weight.any()) and not bool(grads.bias.any())
+    assert ntc.combine(dy, r.weights, ids=r.ids, n_experts=3).shape == (0, 96)
+    drows, dweights = ntc.combine_backward(dy, dy, r.weights, ids=r.ids, n_experts=3)
+    assert drows.shape == (0, 96) and dweights.shape == (0, 2)
