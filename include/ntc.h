@@ -527,8 +527,8 @@ typedef struct {
  * no bin are left untouched.  Products are summed in float32.
  * workspace: >= ntc_linear_workspace_bytes(layer, rows) bytes for the same
  * arguments, 16-byte aligned (NULL if that is 0); contents need not be
- * initialised.  Operands whose rows don't start on 16 bytes (or lie 2^22
- * elements or more apart) or whose in_dim is no multiple of 8 are laid out there
+ * initialised.  Operands whose rows don't start on 16 bytes (or lie more
+ * than 2^22 elements apart) or whose in_dim is no multiple of 8 are laid out there
  * first.  NTC_ERR_ARG, NTC_ERR_CAPACITY (workspace, perm_capacity) as elsewhere;
  * NTC_ERR_UNSUPPORTED where a product would have more than 2^24 - 1 tiles.
  */

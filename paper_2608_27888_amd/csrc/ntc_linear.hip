@@ -297,11 +297,11 @@ Plan plan(Product product, const TileArgs &t) {
       (whole_q && far(t.q_rows, t.q_stride, t.q_width)))
     return {kFar, 128, 0, launched(128)};
   // The tile by what it costs on 256 CUs, in 128 x 128 tiles' worth of MFMA time: a 256
-  // tile fills a CU, two 128 tiles share one at less of its rate (8192 x 4096 x 4096, us
-  // with 256 and 128: forward 213 and 240, input gradient 208 and 272, weight gradient
-  // 193 and 260; forward of 32768 slots, 64 experts, 2048 to 1024: 222 and 228), 64 tiles
-  // come to about half.  Small outputs take the smaller tile that still gives every
-  // CU one.
+  // tile fills a CU, two 128 tiles share one at less of its rate (kernels alone, us with
+  // 256 and 128, 8192 x 4096 x 4096: forward 211 and 240, input gradient 208 and 240, weight
+  // gradient 197 and 232; forward of 32768 slots, 64 experts, 2048 to 1024: 190, its rest
+  // among them, and 196), 64 tiles come to about half.  Small outputs take the smaller tile
+  // that still gives every CU one.
   auto tiles = [&](int64_t side) -> int64_t {
     const int64_t half = (t.n_experts < (int64_t)t.n ? t.n_experts : (int64_t)t.n) / 2 + 1;
     const int64_t rows = product == kWeight ? ((t.rows + side - 1) / side) * t.n_experts
@@ -366,9 +366,10 @@ void start_product(const TileArgs &t, hipStream_t stream) {
 }
 
 // At most 16 rows an expert and tiles of 64 columns for less than half of the CUs: the
-// contraction is what there is to share (4096 x 4096, us here and by 64 tiles: one row
-// 7.6 and 13.3, 16 rows 10.2 and 13.4, 17 rows in two passes 11.5 and 13.7; 8192 x 4096,
-// one row: 15.6 and 13.7).
+// contraction is what there is to share (4096 x 4096, weights in the last-level cache, us
+// here and by 64 tiles: one row 7.6 and 13.3, 16 rows 10.2 and 13.4, 17 rows in two passes
+// 11.5 and 13.7; 8192 x 4096, one row: 15.6 and 13.7.  Weights from memory: 9.0 and 18.9,
+// 11.0 and 19.2, 16.6 and 19.4; 15.6 and 20.1).
 bool few(const TileArgs &t) {
   const int64_t experts = t.n < (uint32_t)t.n_experts ? t.n : t.n_experts;
   return t.n <= 16 * experts && (t.cols + 63) / 64 * experts < 128;

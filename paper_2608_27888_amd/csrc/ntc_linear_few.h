@@ -24,8 +24,8 @@ template <> struct Small<__bf16> {
 // 16 at a time.  Its waves share the contraction: wave w multiplies the blocks of 64
 // values w, w + 8, ... (whole 128-byte lines of every weight row), and the partial sums
 // meet in LDS, added in order.  Bound by the weights' bytes: with 8 waves of up to 16
-// weight loads each a workgroup has 128 KB on their way (4096 x 4096, one row: 7.6 us,
-// 4.4 TB/s).
+// weight loads each a workgroup has 128 KB on their way (4096 x 4096, one row: 9.0 us from
+// memory, 3.7 TB/s; 7.6 from the last-level cache).
 constexpr int kFewWaves = 8;
 
 template <class T>

@@ -327,9 +327,9 @@ __device__ __forceinline__ void find_tile(const TileArgs &a, int log, uint32_t t
 // step after next, spread over more than a half's MFMAs; they have until the next step's
 // first half ends.  One barrier a step covers both.  Steps of 64 and not 32: pieces of
 // whole 128-byte lines (with 64-byte pieces the L2 was asked twice for every line).  At
-// 8192 x 4096 x 4096 bf16 a forward product takes 205 us (1.34 PFLOP/s, MFMA 85 % busy
-// in long contractions; with 64-byte pieces 228), the input gradient 207, the weight
-// gradient 195.  A 64 x 64 tile multiplies a step too fast for the next one's pieces to
+// 8192 x 4096 x 4096 bf16 a forward product takes 211 us (1.30 PFLOP/s, MFMA 85 % busy
+// in long contractions; with 64-byte pieces 228), the input gradient 208, the weight
+// gradient 197.  A 64 x 64 tile multiplies a step too fast for the next one's pieces to
 // come from memory meanwhile: it has four buffers (128 x 4096 x 4096: 32 us with two, 15
 // with four).  MFMA takes Q's rows as its first operand, so a lane ends up with four
 // consecutive output columns of one row.

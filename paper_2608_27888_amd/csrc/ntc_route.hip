@@ -224,7 +224,8 @@ __device__ __forceinline__ void choice_values(const RouteArgs &a, const float (&
         Best<V> best;
         for (int e = g * per; e < (g + 1) * per; ++e) best.join((V)mine.value[e], -INFINITY);
         mine.group[g] = key_of((double)best.worth(a.opt.group_top));
-        if (fuzzy) mine.value[g * per] = (double)best.size(a.opt.group_top);  // read by this lane only
+        // the group's own values have been read, by this lane alone
+        if (fuzzy) mine.value[g * per] = (double)best.size(a.opt.group_top);
       }
       wave_shares();
       for (int g = i; g < G; g += LANES) {
@@ -366,7 +367,7 @@ __device__ __forceinline__ void load_logits(const T *row, int i, int E, bool wid
 // Items are routed by LANES lanes each, up to 256 experts by 16 (four items a wave share
 // every cross-lane step), more by a whole wave.  Bound by instruction issue: the rounds
 // and, with a bias, the exponentials, which are float32 unless two values lie too close
-// (16384 x 256, sigmoid, bias, 8 groups, kernel alone: 20.4 us; with float64 for the whole
+// (16384 x 256, sigmoid, bias, 8 groups, kernel alone: 19.8 us; with float64 for the whole
 // item wherever two of its slots are close 24, for all items 43).
 template <class T, int LANES, int EPL, bool FUZZY, Groups GROUPS>
 __global__ __launch_bounds__(kBlock) void route(RouteArgs a, bool wide) {
@@ -490,7 +491,9 @@ __global__ __launch_bounds__(kBlock) void route(RouteArgs a, bool wide) {
 // LANES lanes per item, lane i holding the experts i EPL .. in registers and, of the k
 // slots, every LANES-th from i on: a weight's share p and the gradient d that reaches its
 // logit directly.  Every expert then collects the d of its slots in ascending order, and
-// with plain softmax weights -s_e sum(p g).  Bound by its bytes.
+// with plain softmax weights -s_e sum(p g).  Bound by instruction issue: 480 vector
+// instructions a wave of four items fill 78 % of the CUs' busy cycles (30001 x 128 bf16, 4
+// slots: 9.2 us, where the bytes would take 3.1).
 template <class T, int LANES, int EPL>
 __global__ __launch_bounds__(kBlock) void route_grad(RouteArgs a, bool wide) {
   constexpr int kItems = kBlock / LANES;

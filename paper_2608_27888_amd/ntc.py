@@ -474,6 +474,10 @@ def freeze_scale(epoch: float, freeze_start: Optional[float], freeze_duration: f
 
 # ----------------------------------------------------------------------------- experts
 
+# Nothing here is recorded by torch's autograd: results carry no history, whether or not the
+# arguments require gradients.  The gradients are calls of their own (*_backward), which a
+# torch.autograd.Function can make.
+
 NTC_OUT_BF16 = 2
 NTC_ACT_NONE, NTC_ACT_GELU, NTC_ACT_SILU = 2, 3, 4
 TYPES = {torch.float32: NTC_OUT_F32, torch.float16: NTC_OUT_F16, torch.bfloat16: NTC_OUT_BF16}
