@@ -551,6 +551,8 @@ int ntc_linear(const ntc_linear_layer *layer, const ntc_linear_rows *rows,
  * grad_format (the layer's type or NTC_OUT_F32), contiguous.  Every element is
  * written: rows and experts without slots get 0.
  * workspace as for ntc_linear, of ntc_linear_backward_workspace_bytes.
+ * NTC_ERR_UNSUPPORTED as for ntc_linear, and where dz is formed or dbias asked for and
+ * dy has more than 2^24 - 1 tiles of 64 slots and 512 columns.
  */
 typedef struct {
   const void *dy;
